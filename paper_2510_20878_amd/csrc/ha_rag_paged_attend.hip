@@ -237,11 +237,12 @@ __device__ __forceinline__ void attend_rows(Params p, const Piece &it, uint32_t 
     for (int x = 0; x < D / 16; ++x) O[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     // Byte offsets, within a head's tile, of where rows lie.  PAGE16 (pages of whole blocks): lane l holds block
-    // group + l's; else token 16 group + l's.  Bad pages count as rows that nobody sees, and are read as page 0.
+    // group + l's; else token 16 group + l's.  Bad pages, and columns beyond the table, count as rows that nobody sees, and are
+    // read as page 0; so are tokens from t1 on, which are not asked for.
     constexpr uint32_t kGroup = PAGE16 ? 64u : 4u;
     auto offset_of = [&](uint32_t tok, uint32_t &lo, uint32_t &hi, bool &bad) {
         const uint32_t col = tok / P, row = tok - col * P;
-        uint32_t page = tok < it.t1 && col < p->n_table ? table[col] : 0u;
+        uint32_t page = tok >= it.t1 ? 0u : col < p->n_table ? table[col] : 0xFFFFFFFFu;
         bad = page >= p->n_pages;
         if (bad) page = 0u;
         const uint64_t off = page * p->page_stride + (uint64_t)row * kRowBytes;
