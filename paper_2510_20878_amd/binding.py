@@ -131,7 +131,7 @@ class HaRagError(RuntimeError):
 
 
 _lib = None
-_float32 = None  # torch's, once the library is loaded
+_float32, _words16 = None, ()  # torch's types, once the library is loaded
 
 
 def lib_path():
@@ -151,8 +151,8 @@ def lib():
         # torch, so the library must bind to that same runtime: import torch first,
         # then the loader resolves libamdhip64 to the copy torch already mapped.
         import torch
-        global _float32
-        _float32 = torch.float32
+        global _float32, _words16
+        _float32, _words16 = torch.float32, (torch.bfloat16, torch.int16)
         L = C.CDLL(path)
         vp, u32, u64, sz = C.c_void_p, C.c_uint32, C.c_uint64, C.c_size_t
         P = C.POINTER
@@ -280,7 +280,7 @@ def paged_step(row_start, slots, n_q_heads, positions=None, refused=None, plan=N
 
 
 def _rows(name, x, n_rows, n_heads, head_dim):
-    """Rows of a tensor [>= n_rows][n_heads][head_dim] of 16-bit words (bfloat16, or int16) with contiguous
+    """Rows of a tensor [>= n_rows][n_heads][head_dim] of bfloat16 (or int16, which hold its words) with contiguous
     dims; a Rows passes through."""
     if type(x) is Rows:
         return x
@@ -289,8 +289,9 @@ def _rows(name, x, n_rows, n_heads, head_dim):
         row, head, dim = x.stride()
     except ValueError:
         n, heads, dims, dim = -1, 0, 0, 0
-    if n < n_rows or heads != n_heads or dims != head_dim or dim != 1 or x.element_size() != 2:
-        raise ValueError(f"{name}: [{n_rows}][{n_heads}][{head_dim}] 16-bit words with contiguous dims wanted, got {tuple(x.shape)}")
+    if n < n_rows or heads != n_heads or dims != head_dim or dim != 1 or x.dtype not in _words16:
+        raise ValueError(f"{name}: [{n_rows}][{n_heads}][{head_dim}] bfloat16 (or int16) with contiguous dims wanted, "
+                         f"got {x.dtype} {tuple(x.shape)}")
     return Rows(x.data_ptr(), row * 2, head * 2)
 
 
