@@ -68,6 +68,7 @@ class AttendRequest(C.Structure):
 
 
 class PagedCache(C.Structure):
+    host = False  # of paged_cache(), page_tables(), paged_step(): a tensor lies where kernels do not reach
     _fields_ = [("base", C.c_void_p), ("page_table", C.c_void_p), ("bad_pages", C.c_void_p),
                 ("page_stride", C.c_uint64), ("tile_stride", C.c_uint64),
                 ("page_tokens", C.c_uint32), ("n_table", C.c_uint32), ("n_pages", C.c_uint32),
@@ -75,12 +76,14 @@ class PagedCache(C.Structure):
 
 
 class PageTables(C.Structure):
+    host = False
     _fields_ = [(n, C.c_void_p) for n in (
         "table", "n_tokens", "n_tokens_after", "free_pages", "n_free", "n_free_after")] + [
             (n, C.c_uint32) for n in ("n_requests", "n_table", "n_pages", "page_tokens")]
 
 
 class PagedStep(C.Structure):
+    host = False
     _fields_ = [(n, C.c_void_p) for n in ("row_start", "slots", "positions", "refused", "plan")] + [
         ("plan_bytes", C.c_uint64)] + [(n, C.c_uint32) for n in (
             "n_requests", "n_rows", "n_q_heads", "reserved")]
@@ -239,8 +242,22 @@ def paged_cache(base, page_table, page_tokens, n_pages, layout, n_layers, n_kv_h
         raise ValueError(layout)
     if n_table is None:
         n_table = page_table.numel() if hasattr(page_table, "numel") else len(page_table)
-    return PagedCache(_addr(base), _addr(page_table), _addr(bad_pages), page_stride, tile_stride,
-                      page_tokens, n_table, n_pages, 0)
+    c = PagedCache(_addr(base), _addr(page_table), _addr(bad_pages), page_stride, tile_stride,
+                   page_tokens, n_table, n_pages, 0)
+    c.host = not all(map(_reached, (base, page_table, bad_pages)))
+    return c
+
+
+def _reached(x):
+    """Whether kernels reach a tensor: it is on the device, or in pinned host memory.  Addresses are taken at their word."""
+    if x is None or isinstance(x, int) or getattr(x, "is_cuda", False):
+        return True
+    return hasattr(x, "is_pinned") and x.is_pinned()
+
+
+def _on_device(name, x, dry=False):
+    if not (dry or x.is_cuda or _reached(x)):
+        raise ValueError(f"{name}: a tensor on the device wanted, its address would fault a kernel")
 
 
 def _ints(name, x, n=None):
@@ -265,6 +282,7 @@ def page_tables(table, n_tokens, free_pages, n_free, page_tokens, n_tokens_after
                    _ints("n_free_after", n_free if n_free_after is None else n_free_after, 1),
                    n_requests, n_table, free_pages.numel(), page_tokens)
     t.tensors = (table, n_tokens, free_pages, n_free, n_tokens_after, n_free_after)  # they live as long as this does
+    t.host = not all(map(_reached, t.tensors))
     return t
 
 
@@ -276,10 +294,11 @@ def paged_step(row_start, slots, n_q_heads, positions=None, refused=None, plan=N
                   _ints("refused", refused, n_requests), _addr(plan),
                   0 if plan is None else plan.numel() * plan.element_size(), n_requests, n_rows, n_q_heads, 0)
     s.tensors = (row_start, slots, positions, refused, plan)
+    s.host = not all(map(_reached, s.tensors))
     return s
 
 
-def _rows(name, x, n_rows, n_heads, head_dim):
+def _rows(name, x, n_rows, n_heads, head_dim, dry):
     """Rows of a tensor [>= n_rows][n_heads][head_dim] of bfloat16 (or int16, which hold its words) with contiguous
     dims; a Rows passes through."""
     if type(x) is Rows:
@@ -292,15 +311,17 @@ def _rows(name, x, n_rows, n_heads, head_dim):
     if n < n_rows or heads != n_heads or dims != head_dim or dim != 1 or x.dtype not in _words16:
         raise ValueError(f"{name}: [{n_rows}][{n_heads}][{head_dim}] bfloat16 (or int16) with contiguous dims wanted, "
                          f"got {x.dtype} {tuple(x.shape)}")
+    _on_device(name, x, dry)
     return Rows(x.data_ptr(), row * 2, head * 2)
 
 
-def _floats(name, x, n):
+def _floats(name, x, n, dry):
     """A contiguous binary32 tensor of at least n elements, or an address."""
     if x is None or type(x) is int:
         return x
     if x.dtype is not _float32 or x.numel() < n or not x.is_contiguous():
         raise ValueError(f"{name}: {n} contiguous float32 values wanted")
+    _on_device(name, x, dry)
     return x.data_ptr()
 
 
@@ -373,6 +394,7 @@ class Context:
                           tau_gpu_ppm, rerank_interval, n_copy_streams, int(dry_run),
                           tau_pin_ppm, tau_page_ppm, 1 if disk_o_direct else 0,
                           1 if half_slots else 0, 1 if pinned_dma else 0, io_threads)
+        self._dry = bool(dry_run)  # no call reaches a kernel
         self._h = C.c_void_p()
         rc = lib().ha_rag_create(C.byref(self.cfg), C.byref(self._h))
         if rc:
@@ -546,13 +568,22 @@ class Context:
     def page_step(self, tables, n_new, step, stream=None):
         """tables: a PageTables (see page_tables()); n_new: int32 [n_requests] on the device; step: a
         PagedStep (see paged_step()), whose arrays are written."""
-        self._chk(lib().ha_rag_page_step(self._h, C.byref(tables), _ints("n_new", n_new, tables.n_requests),
-                                         C.byref(step), _stream(stream)), "ha_rag_page_step")
+        new = _ints("n_new", n_new, tables.n_requests)
+        self._kernels_reach(tables=tables, step=step)
+        if new is not n_new:
+            _on_device("n_new", n_new, self._dry)
+        self._chk(lib().ha_rag_page_step(self._h, C.byref(tables), new, C.byref(step), _stream(stream)), "ha_rag_page_step")
+
+    def _kernels_reach(self, **structures):
+        for name, x in structures.items():
+            if x.host and not self._dry:
+                raise ValueError(f"{name}: tensors on the device wanted, the addresses of others would fault a kernel")
 
     def append_paged(self, k, v, step, cache, layer, stream=None):
         """k, v: BF16 [n_rows][H][D] of any row and head stride; cache: a PagedCache (see paged_cache())."""
         H, D = self.cfg.n_kv_heads, self.cfg.head_dim
-        k, v = _rows("k", k, step.n_rows, H, D), _rows("v", v, step.n_rows, H, D)
+        self._kernels_reach(step=step, cache=cache)
+        k, v = _rows("k", k, step.n_rows, H, D, self._dry), _rows("v", v, step.n_rows, H, D, self._dry)
         self._chk(lib().ha_rag_append_paged(self._h, C.byref(k), C.byref(v), C.byref(step), C.byref(cache), layer,
                                             _stream(stream)), "ha_rag_append_paged")
 
@@ -560,12 +591,13 @@ class Context:
         """q, out: BF16 [n_rows][n_q_heads][D] of any row and head stride; lse, prior_lse: float32
         [n_rows][n_q_heads]; prior_out: float32 [n_rows][n_q_heads][D]; cache: a PagedCache whose page_table is
         [n_requests][n_table] (pass n_table to paged_cache())."""
-        n, Hq, D = step.n_rows, step.n_q_heads, self.cfg.head_dim
-        q, out = _rows("q", q, n, Hq, D), _rows("out", out, n, Hq, D)
+        n, Hq, D, dry = step.n_rows, step.n_q_heads, self.cfg.head_dim, self._dry
+        self._kernels_reach(step=step, cache=cache)
+        q, out = _rows("q", q, n, Hq, D, dry), _rows("out", out, n, Hq, D, dry)
         self._chk(lib().ha_rag_attend_paged(self._h, C.byref(q), C.byref(step), C.byref(cache), layer, sm_scale,
-                                            C.byref(out), _floats("lse", lse, n * Hq),
-                                            _floats("prior_out", prior_out, n * Hq * D),
-                                            _floats("prior_lse", prior_lse, n * Hq), _stream(stream)),
+                                            C.byref(out), _floats("lse", lse, n * Hq, dry),
+                                            _floats("prior_out", prior_out, n * Hq * D, dry),
+                                            _floats("prior_lse", prior_lse, n * Hq, dry), _stream(stream)),
                   "ha_rag_attend_paged")
 
     def register_slab(self, tier, prec, base, nbytes=None):

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2510_20878_amd import binding as B
-from tests.test_paged_step_host import D, H, cache, ctx_of, step
+from tests.test_paged_step_host import D, H, cache, ctx_of, rows, step
 
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.uint16])
@@ -19,3 +19,40 @@ def test_rows_of_other_16_bit_types_are_refused(dtype):
                  lambda: c.attend_paged(bad(16), s, pg, 0, 1.0, good(16)), lambda: c.attend_paged(good(16), s, pg, 0, 1.0, bad(16))):
         with pytest.raises(ValueError, match="bfloat16"):
             call()
+
+
+def test_tensors_in_host_memory_are_refused():
+    """Their addresses would fault a kernel.  (The context below stays dry where it counts: none is launched.)"""
+    c = ctx_of()
+    i32 = lambda *n: torch.zeros(n, dtype=torch.int32)
+    bf = lambda heads: torch.zeros(40, heads, D, dtype=torch.bfloat16)
+    plan = torch.zeros(c.step_plan_bytes(5, 40, 16) + 256, dtype=torch.uint8)
+    plan = plan[-plan.data_ptr() % 256:]
+    there_s, there_pg, there_t = step(c), cache(), B.PageTables(*[1 << 20] * 6, 5, 8, 100, 16)
+    host_s = B.paged_step(i32(6), i32(40), 16, plan=plan)
+    host_t = B.page_tables(i32(5, 8), i32(5), i32(100), i32(1), 16)
+    pool = torch.zeros(1 << 16, dtype=torch.bfloat16)
+    host_pg = B.paged_cache(pool[-(pool.data_ptr() // 2) % 8:], i32(40), 16, 4, "page_major", 3, H, D, n_table=8)
+    table = B.paged_cache(1 << 20, i32(40), 16, 4, "page_major", 3, H, D, n_table=8)
+    here = 1 << 20
+    calls = [lambda: c.page_step(host_t, here, there_s), lambda: c.page_step(there_t, i32(5), there_s),
+             lambda: c.page_step(there_t, here, host_s), lambda: c.append_paged(bf(H), rows(), there_s, there_pg, 0),
+             lambda: c.append_paged(rows(), bf(H), there_s, there_pg, 0), lambda: c.append_paged(rows(), rows(), host_s, there_pg, 0),
+             lambda: c.append_paged(rows(), rows(), there_s, host_pg, 0),
+             lambda: c.attend_paged(bf(16), there_s, there_pg, 0, 1.0, rows(16)),
+             lambda: c.attend_paged(rows(16), there_s, there_pg, 0, 1.0, bf(16)),
+             lambda: c.attend_paged(rows(16), host_s, there_pg, 0, 1.0, rows(16)),
+             lambda: c.attend_paged(rows(16), there_s, table, 0, 1.0, rows(16)),
+             lambda: c.attend_paged(rows(16), there_s, there_pg, 0, 1.0, rows(16), lse=torch.zeros(40, 16)),
+             lambda: c.attend_paged(rows(16), there_s, there_pg, 0, 1.0, rows(16), prior_lse=torch.zeros(40, 16), prior_out=here),
+             lambda: c.attend_paged(rows(16), there_s, there_pg, 0, 1.0, rows(16), prior_out=torch.zeros(40, 16, D), prior_lse=here)]
+    for call in calls:  # a dry context takes them all
+        call()
+    c._dry = False
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError, match="on the device"):
+            call()
+            pytest.fail(f"call {i}")
+    c.page_step(there_t, here, there_s)
+    c.append_paged(rows(), rows(), there_s, there_pg, 0)
+    c.attend_paged(rows(16), there_s, there_pg, 0, 1.0, rows(16), lse=here, prior_out=here, prior_lse=here)
