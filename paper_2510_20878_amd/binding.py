@@ -68,6 +68,7 @@ class AttendRequest(C.Structure):
 
 
 class PagedCache(C.Structure):
+    entries = None  # of the page table's tensor, if it was one: those that requests of n_table entries each may have
     host = False  # of paged_cache(), page_tables(), paged_step(): a tensor lies where kernels do not reach
     _fields_ = [("base", C.c_void_p), ("page_table", C.c_void_p), ("bad_pages", C.c_void_p),
                 ("page_stride", C.c_uint64), ("tile_stride", C.c_uint64),
@@ -245,7 +246,16 @@ def paged_cache(base, page_table, page_tokens, n_pages, layout, n_layers, n_kv_h
     c = PagedCache(_addr(base), _addr(page_table), _addr(bad_pages), page_stride, tile_stride,
                    page_tokens, n_table, n_pages, 0)
     c.host = not all(map(_reached, (base, page_table, bad_pages)))
+    if hasattr(page_table, "numel"):
+        if page_table.is_contiguous():
+            c.entries = page_table.numel()
+        else:  # the first columns of a wider table, whose width n_table has to be
+            wide = page_table.dim() == 2 and page_table.stride() == (n_table, 1)
+            c.entries = len(page_table) * n_table if wide else 0
     return c
+
+
+NOT_REACHED = "tensors on the device wanted, the addresses of others would fault a kernel"
 
 
 def _reached(x):
@@ -253,11 +263,6 @@ def _reached(x):
     if x is None or isinstance(x, int) or getattr(x, "is_cuda", False):
         return True
     return hasattr(x, "is_pinned") and x.is_pinned()
-
-
-def _on_device(name, x, dry=False):
-    if not (dry or x.is_cuda or _reached(x)):
-        raise ValueError(f"{name}: a tensor on the device wanted, its address would fault a kernel")
 
 
 def _ints(name, x, n=None):
@@ -311,7 +316,8 @@ def _rows(name, x, n_rows, n_heads, head_dim, dry):
     if n < n_rows or heads != n_heads or dims != head_dim or dim != 1 or x.dtype not in _words16:
         raise ValueError(f"{name}: [{n_rows}][{n_heads}][{head_dim}] bfloat16 (or int16) with contiguous dims wanted, "
                          f"got {x.dtype} {tuple(x.shape)}")
-    _on_device(name, x, dry)
+    if not (x.is_cuda or dry or _reached(x)):
+        raise ValueError(f"{name}: {NOT_REACHED}")
     return Rows(x.data_ptr(), row * 2, head * 2)
 
 
@@ -321,7 +327,8 @@ def _floats(name, x, n, dry):
         return x
     if x.dtype is not _float32 or x.numel() < n or not x.is_contiguous():
         raise ValueError(f"{name}: {n} contiguous float32 values wanted")
-    _on_device(name, x, dry)
+    if not (x.is_cuda or dry or _reached(x)):
+        raise ValueError(f"{name}: {NOT_REACHED}")
     return x.data_ptr()
 
 
@@ -569,21 +576,20 @@ class Context:
         """tables: a PageTables (see page_tables()); n_new: int32 [n_requests] on the device; step: a
         PagedStep (see paged_step()), whose arrays are written."""
         new = _ints("n_new", n_new, tables.n_requests)
-        self._kernels_reach(tables=tables, step=step)
-        if new is not n_new:
-            _on_device("n_new", n_new, self._dry)
+        dry = self._dry
+        if (tables.host or step.host) and not dry:
+            raise ValueError("tables, step: " + NOT_REACHED)
+        if new is not n_new and not (n_new.is_cuda or dry or _reached(n_new)):
+            raise ValueError("n_new: " + NOT_REACHED)
         self._chk(lib().ha_rag_page_step(self._h, C.byref(tables), new, C.byref(step), _stream(stream)), "ha_rag_page_step")
-
-    def _kernels_reach(self, **structures):
-        for name, x in structures.items():
-            if x.host and not self._dry:
-                raise ValueError(f"{name}: tensors on the device wanted, the addresses of others would fault a kernel")
 
     def append_paged(self, k, v, step, cache, layer, stream=None):
         """k, v: BF16 [n_rows][H][D] of any row and head stride; cache: a PagedCache (see paged_cache())."""
         H, D = self.cfg.n_kv_heads, self.cfg.head_dim
-        self._kernels_reach(step=step, cache=cache)
-        k, v = _rows("k", k, step.n_rows, H, D, self._dry), _rows("v", v, step.n_rows, H, D, self._dry)
+        n, dry = step.n_rows, self._dry
+        if (step.host or cache.host) and not dry:
+            raise ValueError("step, cache: " + NOT_REACHED)
+        k, v = _rows("k", k, n, H, D, dry), _rows("v", v, n, H, D, dry)
         self._chk(lib().ha_rag_append_paged(self._h, C.byref(k), C.byref(v), C.byref(step), C.byref(cache), layer,
                                             _stream(stream)), "ha_rag_append_paged")
 
@@ -592,7 +598,11 @@ class Context:
         [n_rows][n_q_heads]; prior_out: float32 [n_rows][n_q_heads][D]; cache: a PagedCache whose page_table is
         [n_requests][n_table] (pass n_table to paged_cache())."""
         n, Hq, D, dry = step.n_rows, step.n_q_heads, self.cfg.head_dim, self._dry
-        self._kernels_reach(step=step, cache=cache)
+        if (step.host or cache.host) and not dry:
+            raise ValueError("step, cache: " + NOT_REACHED)
+        if cache.entries is not None and step.n_requests * cache.n_table > cache.entries:
+            raise ValueError(f"cache: {step.n_requests} requests of {cache.n_table} entries each wanted, "
+                             f"the page table has {cache.entries}: pass n_table to paged_cache()")
         q, out = _rows("q", q, n, Hq, D, dry), _rows("out", out, n, Hq, D, dry)
         self._chk(lib().ha_rag_attend_paged(self._h, C.byref(q), C.byref(step), C.byref(cache), layer, sm_scale,
                                             C.byref(out), _floats("lse", lse, n * Hq, dry),

@@ -56,3 +56,20 @@ def test_tensors_in_host_memory_are_refused():
     c.page_step(there_t, here, there_s)
     c.append_paged(rows(), rows(), there_s, there_pg, 0)
     c.attend_paged(rows(16), there_s, there_pg, 0, 1.0, rows(16), lse=here, prior_out=here, prior_lse=here)
+
+
+def test_page_tables_of_fewer_entries_than_the_requests_read_are_refused():
+    """Without n_table a cache is one request's, of all entries: request r's would begin r times the whole table behind its start."""
+    c = ctx_of()
+    s, table = step(c), torch.zeros(5, 8, dtype=torch.int32)
+    pg = lambda t, **kw: B.paged_cache(1 << 20, t, 16, 100, "page_major", 3, H, D, **kw)
+    c.attend_paged(rows(16), s, pg(table, n_table=8), 0, 1.0, rows(16))
+    c.attend_paged(rows(16), s, pg(table[:, :6].contiguous(), n_table=6), 0, 1.0, rows(16))
+    c.attend_paged(rows(16), s, pg(1 << 20, n_table=8), 0, 1.0, rows(16))  # an address is taken at its word
+    c.attend_paged(rows(16), s, pg(table[:, :6], n_table=8), 0, 1.0, rows(16))
+    for cache_ in (pg(table), pg(table, n_table=9), pg(table[:4], n_table=8), pg(table[:, :6], n_table=6), pg(table[:4, :6], n_table=8),
+                   pg(table.T, n_table=5), pg(table.flatten()[::2], n_table=4)):
+        with pytest.raises(ValueError, match="n_table"):
+            c.attend_paged(rows(16), s, cache_, 0, 1.0, rows(16))
+    one = step(c, n_requests=1)
+    c.attend_paged(rows(16), one, pg(table[0]), 0, 1.0, rows(16))
