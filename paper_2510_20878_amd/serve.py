@@ -52,7 +52,8 @@ def _reference(ctx, shape, docs, pool, table, held, q, layer, tokens, P):
 
 def serve(n_requests=8, n_steps=16, n_layers=4, kv_heads=8, q_heads=32, head_dim=128, doc_tokens=512, n_docs=32, per_request=4,
           question=(48, 17, 64, 33), answer=24, page_tokens=16, seed=0, check=False):
-    """Runs the loop; returns (seconds a step, largest error of the last step over the size of its output or None)."""
+    """Runs the loop; returns (seconds a step that has rows, largest error of the last step over the size of its output; None without check, or if
+    no request had rows in that step)."""
     shape = L, H, D = n_layers, kv_heads, head_dim
     P, scale = page_tokens, head_dim ** -0.5
     g = torch.Generator(device="cuda").manual_seed(seed)
@@ -77,7 +78,7 @@ def serve(n_requests=8, n_steps=16, n_layers=4, kv_heads=8, q_heads=32, head_dim
 
     age = [-(i % 3) for i in range(n_requests)]  # steps that the request has seen; < 0: it has not come yet
     docs = [[(i * 7 + j) % n_docs for j in range(per_request)] for i in range(n_requests)]
-    spent, error = 0.0, None
+    spent, worked, error = 0.0, 0, None
     for nth in range(n_steps):
         # what the scheduler decides, on the host: who brings a question, who decodes, who has ended
         new = [question[i % len(question)] if a == 0 else 1 if 0 < a < answer else 0 for i, a in enumerate(age)]
@@ -90,6 +91,10 @@ def serve(n_requests=8, n_steps=16, n_layers=4, kv_heads=8, q_heads=32, head_dim
         q = q.contiguous()
         first = [sum(new[:i]) for i in range(n_requests)]
         live = [i for i in range(n_requests) if new[i]]
+        error = None
+        if not live:  # one has ended and the next has not come yet
+            age = [a + 1 for a in age]
+            continue
         requests = [ctx.attend_id_lists([(docs[i], q[layer, first[i]:], prior[first[i]:], prior_lse[first[i]:], new[i]) for i in live])
                     for layer in range(L)]
         ws = torch.empty(max(ctx.attend_chunks_workspace_bytes(requests[0], q_heads), 16), dtype=torch.uint8, device="cuda")
@@ -101,7 +106,7 @@ def serve(n_requests=8, n_steps=16, n_layers=4, kv_heads=8, q_heads=32, head_dim
             ctx.attend_chunks(requests[layer], layer, q_heads, scale, ws, count=layer == 0)
             ctx.attend_paged(q[layer], step, cache, layer, scale, out[layer], prior_out=prior, prior_lse=prior_lse)
         torch.cuda.synchronize()
-        spent += time.perf_counter() - began
+        spent, worked = spent + time.perf_counter() - began, worked + 1
         assert not refused.any(), "the pool holds every request's longest conversation"
         if check and nth == n_steps - 1:
             error = 0.0
@@ -120,7 +125,7 @@ def serve(n_requests=8, n_steps=16, n_layers=4, kv_heads=8, q_heads=32, head_dim
         age = [-1 if i in ended else a + 1 for i, a in enumerate(age)]
     torch.cuda.synchronize()
     ctx.destroy()
-    return spent / n_steps, error
+    return spent / max(worked, 1), error
 
 
 def main(argv=None):

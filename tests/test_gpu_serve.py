@@ -21,3 +21,11 @@ def test_serving_loop_other_shape():
     _, error = serve.serve(n_requests=3, n_steps=9, n_layers=1, kv_heads=2, q_heads=14, doc_tokens=64, n_docs=6, per_request=2,
                            question=(200, 5), answer=6, page_tokens=12, check=True)
     assert error < LIMIT, error
+
+
+@pytest.mark.parametrize("steps,live", [(6, False), (7, True), (12, False), (20, True)])
+def test_serving_loop_of_one_request_that_ends(steps, live):
+    """Steps 0 to 4 answer, step 5 has no rows, steps 6 to 10 answer the next one's question, and so on."""
+    _, error = serve.serve(n_requests=1, n_steps=steps, n_layers=1, doc_tokens=64, n_docs=4, per_request=2, question=(9,), answer=5,
+                           check=True)
+    assert error < LIMIT if live else error is None, error
