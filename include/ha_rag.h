@@ -568,7 +568,7 @@ int ha_rag_append_paged(ha_rag_ctx *ctx, const ha_rag_rows *k, const ha_rag_rows
  * out overlaps none of what is read.  Scores and sums are binary32; the softmax weights are rounded to BF16 before they multiply v, and out is
  * normalised by the sum of the rounded ones.
  * A plan that ha_rag_page_step has not written for this n_requests, n_rows, n_q_heads and shape leaves everything unwritten.
- * EFORMAT unless head_dim is 64, 96 or 128; EINVAL, ENOSPC as above, and for sm_scale <= 0. */
+ * EFORMAT unless head_dim is 64, 96 or 128; EINVAL, ENOSPC as above, and for sm_scale <= 0 or >= 1e30. */
 int ha_rag_attend_paged(ha_rag_ctx *ctx, const ha_rag_rows *q, const ha_rag_paged_step *step,
                         const ha_rag_paged_cache *cache, uint32_t layer, float sm_scale, const ha_rag_rows *out,
                         float *lse, const float *prior_out, const float *prior_lse, void *stream);

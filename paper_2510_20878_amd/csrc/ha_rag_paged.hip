@@ -175,7 +175,7 @@ int ha_rag_attend_paged(ha_rag_ctx *c, const ha_rag_rows *q, const ha_rag_paged_
     StepLayout lay;
     int rc = check_step(c, s, &lay);
     if (rc) return rc;
-    if (!rows_ok(q) || !rows_ok(out) || layer >= c->cfg.n_layers || !(sm_scale > 0.0f)) return HA_RAG_EINVAL;
+    if (!rows_ok(q) || !rows_ok(out) || layer >= c->cfg.n_layers || !(sm_scale > 0.0f) || !(sm_scale < 1e30f)) return HA_RAG_EINVAL;
     if (!aligned(lse, 4) || !aligned(prior_out, 16) || !aligned(prior_lse, 4) || !prior_out != !prior_lse) return HA_RAG_EINVAL;
     if ((rc = check_pool(cache)) != HA_RAG_OK) return rc;
     if (!cache->page_table || !aligned(cache->page_table, 4) || cache->n_table == 0) return HA_RAG_EINVAL;

@@ -73,3 +73,14 @@ def test_page_tables_of_fewer_entries_than_the_requests_read_are_refused():
             c.attend_paged(rows(16), s, cache_, 0, 1.0, rows(16))
     one = step(c, n_requests=1)
     c.attend_paged(rows(16), one, pg(table[0]), 0, 1.0, rows(16))
+
+
+def test_scales_beyond_the_range_are_refused():
+    """As attend_packed refuses them: times log2 e they leave binary32, and every score is infinite or no number."""
+    c = ctx_of()
+    s, pg = step(c), cache()
+    c.attend_paged(rows(16), s, pg, 0, 9e29, rows(16))
+    for scale in (1e30, 3.4e38, float("inf"), float("nan"), -float("inf")):
+        with pytest.raises(B.HaRagError) as e:
+            c.attend_paged(rows(16), s, pg, 0, scale, rows(16))
+        assert e.value.code == B.EINVAL, scale
