@@ -488,7 +488,8 @@ int ha_rag_attend_chunks_workspace_bytes(ha_rag_ctx *ctx, const uint64_t *ids,
  * (ha_rag_append_paged), and the new tokens attend to what their request holds (ha_rag_attend_paged), merged with
  * the attention over its packed documents (ha_rag_attend_packed, ha_rag_attend_chunks) if there is one.  All lengths,
  * tables and page ids are on the device; the calls only launch kernels on `stream`, so a step
- * may be recorded into a HIP graph and replayed. */
+ * may be recorded into a HIP graph and replayed.  The attention of a step's layers shares the step's plan (counters, partial
+ * results): ha_rag_attend_paged calls with one plan follow one another, on one stream or with events between. */
 #define HA_RAG_MAX_PAGED_REQUESTS 4096
 #define HA_RAG_NO_PAGE UINT32_MAX
 
@@ -512,7 +513,8 @@ typedef struct ha_rag_paged_step {
     int32_t *positions;   /* nullable [n_rows] the row's index in its request, or -1                     */
     uint32_t *refused;    /* nullable [n_requests] 1 = the request's new rows found no room               */
     void *plan;           /* ha_rag_step_plan_bytes() bytes, 256-byte aligned: how the attention is cut, and its
-                             partial results.  Steps that run side by side need one each          */
+                             partial results.  One call at a time uses it: steps that run side by side need one
+                             each, and two layers of one step cannot run side by side            */
     uint64_t plan_bytes;
     uint32_t n_requests;  /* 1..HA_RAG_MAX_PAGED_REQUESTS                                                */
     uint32_t n_rows;      /* rows that the arrays have room for, 1 or more                               */
@@ -563,7 +565,7 @@ int ha_rag_append_paged(ha_rag_ctx *ctx, const ha_rag_rows *k, const ha_rag_rows
  * attention of the same rows over other keys, such as ha_rag_attend_packed's, that the result is merged
  * with; where prior_lse is -inf there is none, and prior_out is not used.  A row that sees nothing gets out = 0 and lse =
  * -inf; so do rows of refused requests, if there is no prior.  Rows beyond the last request's are not written.
- * Keys and values of the rows held must be finite; what lies in other rows of the pool does not matter.  Rows in a page that is
+ * Queries, and keys and values of the rows held, must be finite; what lies in other rows of the pool does not matter.  Rows in a page that is
  * >= n_pages, or beyond cache->n_table, count as not there, and bad_pages is added to.
  * out overlaps none of what is read.  Scores and sums are binary32; the softmax weights are rounded to BF16 before they multiply v, and out is
  * normalised by the sum of the rounded ones.

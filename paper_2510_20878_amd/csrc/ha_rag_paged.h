@@ -14,7 +14,11 @@ constexpr uint32_t kStepMagic = 0x53544550u;  // the first word of a plan that k
 // are counted in units.  The tiles of all requests, one after the other, are a line, the same for every KV head: each tile
 // has a place of kTileUnits units for what it costs to begin and end it, then those of its tokens.
 //   cut:    the line is cut into runs of `run` units, one per workgroup and head, wherever that falls: every workgroup has the
-//           same to read.  A tile that lies in several runs gets one partial result of each.
+//           same to read where tiles see what their request holds, as in decode.  A tile that lies in several runs gets one partial
+//           result of each.  (Every tile of a request counts the units of all rows held, but sees those up to its last row.  A chunk
+//           over much less than its own length is therefore shared out unevenly: of a prompt of 2,000 rows from nothing, 8 x 4
+//           heads, the busiest workgroup works on 32 units, the mean is 16; 62 us, where a chunk of 2,000 over 2,000, which is three
+//           times as much, takes 150.  Pieces of rows that a tile does not see are written and joined like others.)
 //   whole:  each tile has a workgroup of its own, in request order, the last tile of a request (which sees most) first; where there
 //           are enough of them, and of such lengths, that this comes out about even (k9_page_scan says when).
 struct StepHdr {
@@ -70,9 +74,10 @@ constexpr uint32_t kLeastRun = 7;     // units: shorter runs cost more to join t
 constexpr uint32_t kManyTiles = 3;    // tiles of 16 rows are taken whole from so many times more of them than workgroups that run at once
 
 // A step's layers come one after the other, and what one leaves in the last-level cache (256 MB) is of use only if the keys and values of
-// all of them fit there until the next step.  Beyond this many bytes they are read past it.  Decode of 32 requests over 5,000 rows
-// each (671 MB a layer) takes 126 us through the cache and 114 past it, of 128 requests 454 and 415; of 4 requests (86 MB a layer,
-// two layers), called again and again, 25.7 and 29.1.
+// all of them fit there until the next step.  Beyond this many bytes they are read past it.  us a layer of decode over 5,000 rows a
+// request (20.5 MB), layers in turn, through the cache / past it: 128 requests 416 / 381, 32 requests of two layers 115 / 102, of one
+// layer 109 / 97, 18 requests (369 MB in all) 66.4 / 61.3, 16 (328 MB) 57.2 / 54.4, 14 (287 MB) 48.7 / 49.3, 8 requests of two layers
+// (328 MB) 33.5 / 32.8, 4 of four 22.2 / 22.0, 4 of two (164 MB) 21.2 / 21.3: even below the border, and past it from there on.
 constexpr uint64_t kPastBytes = 320ull << 20;
 
 struct K9Params {

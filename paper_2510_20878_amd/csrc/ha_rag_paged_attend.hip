@@ -12,7 +12,9 @@
 // out = o / l, lse = r + log l.  Two such results over different tokens join as r = max, o = o1 exp(r1 - r) + o2 exp(r2 - r), l
 // likewise: waves of a workgroup, pieces of a tile and the prior attention are joined so.  Scores, references and sums are
 // binary32.  The weights are rounded to BF16 because the matrix instructions that multiply v take no more; out is divided by
-// the sum of the rounded ones (so rounding does not scale it), the lse keeps the unrounded sum.
+// the sum of the rounded ones (so rounding does not scale it), the lse keeps the unrounded sum.  Against 64 bits out is off by 1.9e-3 of its
+// norm, of which 1.6e-3 to 1.7e-3 are its own rounding to BF16; a second product with what the weights lose would save the rest for twice
+// the matrix instructions of O, which tiles of 128 rows have no room for and which would leave the two forms unlike.
 //
 // Tiles of 16 rows (attend_rows).  Bound: HBM.  Every wave reads its own share of the tokens, 16 at a time, straight into
 // registers, one block on its way while one is worked on; no LDS until the waves are joined.  Scores are computed
@@ -20,12 +22,14 @@
 // is how rows lie in memory, and receives the scores of tokens 4 c .. 4 c + 3 for query row n: the layout in which P^T is
 // the second operand of O^T = V^T P^T (16x16x16 MFMA).  V's operand is 4 tokens of one dim: the lane loads D / 16 neighbouring
 // dims of its tokens 4 c + i and regroups them by pairs.  Measured: 32 requests of 5,130 rows, 8 KV heads of 128, 105 us (6.4 TB/s);
-// one of 131,072 rows 89 us (6.0); 48 of 900 rows, 32 KV heads, pages of 12 rows, 129 us (5.5).
+// one of 131,072 rows 88 us (6.1); 48 of 900 rows, 32 KV heads, pages of 12 rows, 129 us (5.5).  Heads of 64 and 96, 32 requests of 5,130
+// rows: 62.5 us (5.4) and 90 us (5.6).
 //
 // Tiles of 128 rows (attend_tiles).  Bound: the matrix and the vector unit, which share their SIMD's issue.  A wave owns 32 rows
 // (32x32x16 MFMA, S^T and O^T as above); keys and values of 64 tokens at a time go to LDS past the registers for all four waves.
-// Measured: chunks of 517 to 1,024 rows over up to 5,120, 64 query heads on 8, 316 to 330 us (890 to 920 TFLOP/s of 1,256 that a product
-// of 8,192 x 8,192 matrices reaches); 24 questions of 5 to 64 rows over 16 to 2,112, 43 us.  Where that goes, of 320 us with parts
+// Measured: chunks of 517 to 1,024 rows over up to 5,120, 64 query heads on 8, 315 to 345 us, by card (850 to 925 TFLOP/s of 1,256 that a product
+// of 8,192 x 8,192 matrices reaches); 24 questions of 5 to 64 rows over 16 to 2,112, 43 us in a graph.  Heads of 64 and 96, chunks of 1,024 over 4,096: 709
+// and 843 TFLOP/s (of 128: 927), since exponentials are as many and products fewer.  Where that goes, of 320 us with parts
 // left out: exponentials and sums 35, the second product 68, the loads to LDS 40; the matrix unit is busy 41 % of the
 // clocks, the vector unit 49 %, LDS 21 % and free of bank conflicts.
 #include "ha_rag_attend_dev.h"

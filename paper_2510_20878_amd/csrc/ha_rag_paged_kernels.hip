@@ -240,19 +240,31 @@ __global__ __launch_bounds__(kScanThreads) void k9_page_scan(const K9Params p)
     block_exclusive(x6, sum6, all6);
     uint32_t work_ex = x6[1];
     const uint32_t n_taken = all6[0], n_tiles = all6[2], n_units = all6[3], n_seen = all6[4], n_units16 = all6[5];
-    // Whole tiles.  Large ones where none takes longer than a run would, so that taking them in turn comes out about even: their partial
-    // results, 64 KiB each way, are saved.  us cut / whole: two chunks of 1,000 rows (127 tiles, the longest 0.7 of a run) 305 / 267, three
-    // 333 / 289, four 366 / 323; 40 questions (67 tiles, 2.5) 57 / 62, 96 (160 tiles, 1.06) 115 / 118.  Tiles of 16 rows, whose partial
-    // results are small, where they are many and short: 1,000 requests of 200 rows 180 / 170, of 40 90 / 80; 60 of 900 rows and 32
-    // heads 158 / 174, 256 of 5,000 806 / 916.  (A line that 32 bits do not hold is not cut.)
+    // Whole tiles, or runs.  All figures: 8 KV heads of 128, 4 query heads each, pages of 16 rows, us cut / whole in a graph.
+    // Tiles of 16 rows, whose partial results are small: whole from more than 3 times as many as workgroups that run at once (64 a
+    // head), if they count less than 12 units on average (550 rows).  224 tiles of 100 rows 29.7 / 25.1, of 400 73.5 / 69.4, of 550
+    // 93.1 / 88.3, of 1,500 225 / 219, of 2,500 359 / 373; 192 of 100 24.3 / 22.2, of 400 59.4 / 59.5, of 1,000 127 / 129; 300 of 1,500 299 / 302;
+    // 1,000 of 100 129 / 117, of 400 315 / 304.  Just beyond the borders the choice costs 5 to 9 %; far fewer tiles come out
+    // even only where their number happens to go into that of the workgroups (160 of 100 rows 24.3 / 20.1, 100 of 1,500 108 / 115).
+    // Large ones (64 KiB of partial results each way) where there are more than workgroups and none takes longer than a run
+    // would: four chunks of 1,000 rows over 1,000 144 / 133, 16 of 160 over 1,000 84 / 75, 5 of 1,000 over 100 107 / 84.  The longest may
+    // be 1.0 of a run (three of 1,000 over 1,500 to 6,000 253 / 226) and 1.2 (16 of 160 over 500 to 2,000 94 / 85) before it is even (1.3, 40 of 48
+    // rows over 500 to 2,000 83 / 86) and lost (1.5, 70 of 30 rows over 1,000 to 4,000 174 / 187): the border is on the safe side.
+    // That rule is for steps whose large tiles have two thirds of the units: 32 requests of one row and 16 of 100, over 500, 56 / 43.  With
+    // fewer, the few long ones may end last (16 of one row and one of 100, over 2,500, 48 to 55 / 60) or not (64 and 16, over 500, 61 / 53;
+    // 64 and 8 49 / 49): all cut.
+    // (A line that 32 bits do not hold is not cut.)
     const bool small = n_units16 >= n_units / 3u;
     const bool whole = n_units == 0xFFFFFFFFu || (small ? n_tiles > kManyTiles * p.lay.target && n_units / 12u < n_tiles
                                                         : n_tiles > p.lay.target && longest <= n_units / p.lay.target);
     // Streaming (tiles of 16 rows, pages of whole blocks) is fastest with one workgroup a compute unit; a second one hides what happens
-    // between two tiles, and matters where tiles are short and a workgroup has several.  us with one / two, KV heads 8: 32 requests of 5,000
-    // rows 107 / 115, 96 310 / 326, one of 131,072 rows 89 / 97, 64 of 2,500 102 / 105; 64 of 1,200 57 / 57, 128 of
-    // 1,200 110 / 103; 28 of 1,000 and 4 with 40 new rows (36 tiles) 209 / 217, twice as many 375 / 327.  Pages of 12 rows: 48 requests of 4,000
-    // rows, 32 heads, 512 / 499.  Large tiles alone (40 of them, 11 units each) 57 / 50.
+    // between two tiles, and matters where tiles are short and a workgroup has several.  us with one / two: 32 requests of 400
+    // rows 14.3 / 19.4, of 5,000 102 / 114, 40 of 1,500 43.3 / 44.6, 48 of 1,000 36.9 / 39.9, 64 of 200 17.0 / 15.4, of 1,000 44.9 / 43.7, of 1,500
+    // 64.1 / 65.7, of 2,500 101 / 105, 160 of 200 35.4 / 30.5, of 1,000 110 / 115, of 2,500 248 / 262, 300 of 700 154 / 152, of 1,500
+    // 288 / 299.  So: one where there are few tiles (five eighths of the workgroups that run at once; it is even between that and as many)
+    // and where they are long (32 units on average; it is even between 14 and 27).  A few large tiles among them gain from two (64 requests
+    // of one row and 4 of 100, over 2,500, 154 / 140).  Pages of 12 rows: 48 requests of 4,000 rows, 32 heads, 512 / 499.  Large tiles
+    // alone (40 of them, 11 units each) 57 / 50.
     const bool one = P % 16u == 0 && small && (n_tiles <= p.lay.target * 5u / 8u || n_units / 32u >= n_tiles);
     const uint32_t target = one ? max(p.lay.target / 2u, 1u) : p.lay.target;
     const uint32_t run = whole ? 0u : max(n_units / target + (n_units % target != 0u), kLeastRun);
