@@ -295,6 +295,8 @@ def paged_step(row_start, slots, n_q_heads, positions=None, refused=None, plan=N
     """A PagedStep: row_start [n_requests + 1], slots and positions [n_rows], refused [n_requests]: int32
     tensors on the device; plan: Context.step_plan_bytes() bytes there."""
     n_requests, n_rows = row_start.numel() - 1, slots.numel()
+    if hasattr(plan, "is_contiguous") and not plan.is_contiguous():
+        raise ValueError("plan: contiguous bytes wanted")
     s = PagedStep(_ints("row_start", row_start), _ints("slots", slots), _ints("positions", positions, n_rows),
                   _ints("refused", refused, n_requests), _addr(plan),
                   0 if plan is None else plan.numel() * plan.element_size(), n_requests, n_rows, n_q_heads, 0)

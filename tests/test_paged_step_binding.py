@@ -84,3 +84,12 @@ def test_scales_beyond_the_range_are_refused():
         with pytest.raises(B.HaRagError) as e:
             c.attend_paged(rows(16), s, pg, 0, scale, rows(16))
         assert e.value.code == B.EINVAL, scale
+
+
+def test_plans_that_hold_fewer_bytes_than_they_count_are_refused():
+    i32 = lambda *n: torch.zeros(n, dtype=torch.int32)
+    plan = torch.zeros(1 << 16, dtype=torch.uint8)
+    assert B.paged_step(i32(6), i32(40), 16, plan=plan.view(torch.int64)).plan_bytes == 1 << 16
+    for bad in (plan[:1].expand(1 << 16), plan[::2]):
+        with pytest.raises(ValueError, match="plan"):
+            B.paged_step(i32(6), i32(40), 16, plan=bad)
